@@ -54,9 +54,11 @@ __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_
 template <int LEFT>
 __device__ __forceinline__ void copies_wait_but() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
-// Codes are read once: they take no room in L1.
+// Codes are read once: they take no room in L1.  The kernel before this one in the stream may have written them, and may still be running when this one
+// starts: volatile, so that the load stays behind wait_for_launch_before, and coherent, as all loads here are (a non-coherent one is for what nobody writes
+// while a kernel lives).
 __device__ __forceinline__ void load_codes(uint32_t* w, const uint32_t* p) {  // 16 bytes
-  asm("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
 }
 
 __device__ __forceinline__ uint32_t mask_or(uint32_t w, uint32_t mask, uint32_t set) {  // (w & mask) | set in one instruction
@@ -213,10 +215,10 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) packed_matvec_kernel(MatvecA
             if constexpr (LW == 4) {
               load_codes(ww[i][h], at);
             } else if constexpr (LW == 2) {
-              const uint2 x = __ldg(reinterpret_cast<const uint2*>(at));
+              const uint2 x = *reinterpret_cast<const uint2*>(at);
               ww[i][h][q] = x.x; ww[i][h][q + 1] = x.y;
             } else {
-              ww[i][h][q] = __ldg(at);
+              ww[i][h][q] = *at;
             }
           }
       }
@@ -256,10 +258,10 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) packed_matvec_kernel(MatvecA
       if (s < chunk_slabs && slab < s1 && col < a.cols) {
         const unsigned char* p = static_cast<const unsigned char*>(a.x) + ((int64_t)(m0 + m) * a.ldx + col) * ELEM;
         if (col + 8 <= a.cols && (reinterpret_cast<uintptr_t>(p) & 15u) == 0) {
-          const uint4 q0 = __ldg(reinterpret_cast<const uint4*>(p));
+          const uint4 q0 = *reinterpret_cast<const uint4*>(p);
           raw[k][0] = q0.x; raw[k][1] = q0.y; raw[k][2] = q0.z; raw[k][3] = q0.w;
           if constexpr (TYPE == LPC_F32) {
-            const uint4 q1 = __ldg(reinterpret_cast<const uint4*>(p) + 1);
+            const uint4 q1 = reinterpret_cast<const uint4*>(p)[1];
             raw[k][4] = q1.x; raw[k][5] = q1.y; raw[k][6] = q1.z; raw[k][7] = q1.w;
           }
         } else {
@@ -587,10 +589,10 @@ __global__ void __launch_bounds__(MT, PIECES<TYPE> * MP <= 16 ? 2 : 1) packed_ma
         const unsigned char* p = ys[v] + r0 * ELEM;
         if (fast[v] && r0 + 4 <= a.rows) {
           if constexpr (P == 3) {
-            const uint4 q = __ldg(reinterpret_cast<const uint4*>(p));
+            const uint4 q = *reinterpret_cast<const uint4*>(p);
             y[v][0] = q.x; y[v][1] = q.y; y[v][2] = q.z; y[v][3] = q.w;
           } else {
-            const uint2 q = __ldg(reinterpret_cast<const uint2*>(p));
+            const uint2 q = *reinterpret_cast<const uint2*>(p);
             y[v][0] = q.x; y[v][1] = q.y;
           }
         } else {
