@@ -148,6 +148,9 @@ struct MatvecPlan {
 // vector two (11 bits each and the sign of the second: 2^-24 of a value is lost, half a step of fp32).  What falls out of fp16's
 // range at the lower end is below 2^-39 of the largest of the 128.  Where one of the 128 is not finite, every product with them is
 // infinite or NaN whatever the others are: those are taken as zeros, so that none of them overflows.
+// Small vectors are multiplied by much, and a sum of 128 products, up to 2^25 then, times a large scale could leave the floats though the result does not:
+// the factor f that undoes the power is taken in two parts, f1 = f but 2^-26 at least and 1 at most before the scale, f2 = f / f1 behind it.  Where f is below
+// 1 the first product is below the scale and the second one smaller still; where it is not, what overflows does so rightly.
 //
 // 16384 x 16384, groups of 128: 33 us for one vector (4.3 TB/s; 24 us with nothing to read, 28 us with a quarter of the arithmetic: both sides
 // overlap, but not fully with the 16 warps an SM that the registers allow), 43 us for 8, 57 us for 16, where laying out the
@@ -178,7 +181,7 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) packed_matvec_kernel(MatvecA
   // shared memory: two buffers of vectors, their factors
   uint4* sx = reinterpret_cast<uint4*>(smem);
   const int sx_size = chunk_slabs * 16 * NC;
-  float* factor = reinterpret_cast<float*>(sx + 2 * sx_size);
+  float2* factor = reinterpret_cast<float2*>(sx + 2 * sx_size);  // f1 and f2
   float* red = reinterpret_cast<float*>(smem);
 
   // ---- codes, PD slabs ahead.  Behind the last row the last one is read again (its result is not kept); what is behind a row's last word stays
@@ -229,7 +232,7 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) packed_matvec_kernel(MatvecA
 
   // ---- scales: those of 16 parts of 32 LW columns at a time, a row's next to each other in memory and the rows' next to each other in shared memory
   constexpr int PARTS = 16, SROW = ROWS + 1, SCALE_TURNS = PARTS / NG / WK;
-  float* sd = factor + 2 * chunk_slabs * M;
+  float* sd = reinterpret_cast<float*>(factor + (TYPE == LPC_F16 ? 0 : 2 * chunk_slabs * M));
   auto bring_scales = [&](int stretch) {
     const int part = threadIdx.x & ((1 << plan.parts_log2) - 1), p = s0 * NG + stretch * PARTS + part;  // as many threads to a row as there are parts
     if (p >= min(parts, s1 * NG)) return;
@@ -279,7 +282,7 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) packed_matvec_kernel(MatvecA
   };
   auto lay_out = [&](int chunk) {
     uint4* to = sx + (chunk & 1) * sx_size;
-    float* fto = factor + (chunk & 1) * chunk_slabs * M;
+    float2* fto = factor + (chunk & 1) * chunk_slabs * M;
     int s = s_first, m = m_first;
 #pragma unroll
     for (int k = 0; k < TASKS; ++k) {
@@ -290,7 +293,6 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) packed_matvec_kernel(MatvecA
             const uint32_t* v = raw[k];
             to[((s * 4 + lq) * NC + m) * 4 + lt] = make_uint4(__byte_perm(v[0], v[2], 0x5410u), __byte_perm(v[0], v[2], 0x7632u),
                                                               __byte_perm(v[1], v[3], 0x5410u), __byte_perm(v[1], v[3], 0x7632u));
-            if (word == 0) fto[s * M + m] = 1.f;
           }
         } else {
           float x[8];
@@ -310,7 +312,6 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) packed_matvec_kernel(MatvecA
           const bool all_finite = top < 0x7F800000u;
           const int ex = max((int)(top >> 23), 15);  // 2^(127 + 14 - ex) is a float from there on
           const float up = all_finite ? __uint_as_float((uint32_t)(268 - ex) << 23) : 1.f;
-          const float down = all_finite ? __uint_as_float((uint32_t)(ex - 14) << 23) : 1.f;
           __half2 hi[4], lo[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
@@ -325,7 +326,10 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) packed_matvec_kernel(MatvecA
           if (mine) {
             to[((s * 4 + lq) * NC + m) * 4 + lt] = *reinterpret_cast<uint4*>(hi);
             if constexpr (P == 2) to[((s * 4 + lq) * NC + M + m) * 4 + lt] = *reinterpret_cast<uint4*>(lo);
-            if (word == 0) fto[s * M + m] = down;
+            if (word == 0) {
+              const int down = all_finite ? ex - 14 : 127, first = min(max(down, 127 - 26), 127);  // exponent fields of f and f1
+              fto[s * M + m] = make_float2(__uint_as_float((uint32_t)first << 23), __uint_as_float((uint32_t)(127 + down - first) << 23));
+            }
           }
         }
       }
@@ -361,7 +365,7 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) packed_matvec_kernel(MatvecA
     bring(chunk + 1);  // behind the last chunk: zeros, nothing is read
     const float* ds = sd + ((stretch & 1) * PARTS + (turn0 % SCALE_TURNS * WK + wk) * NG) * SROW + wr * RT * 16 + g;
     const uint4* xs = sx + (chunk & 1) * sx_size + (size_t)wk * 16 * NC + t;
-    const float* fs = factor + (chunk & 1) * chunk_slabs * M + wk * M;
+    const float2* fs = factor + (chunk & 1) * chunk_slabs * M + wk * M;
     for (int turn1 = turn0; turn1 < min(turn0 + plan.chunk, turns); turn1 += PD) {
 #pragma unroll
       for (int u = 0; u < PD; ++u) {
@@ -401,15 +405,17 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) packed_matvec_kernel(MatvecA
 #pragma unroll
               for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  sum[i][n][e] = k == 0 ? mul_rn(e < 2 ? d0 : d1, acc[i][n][e]) : __fmaf_rn(e < 2 ? d0 : d1, acc[i][n][e], sum[i][n][e]);
+                for (int e = 0; e < 4; ++e) {
+                  const float part = TYPE == LPC_F16 ? acc[i][n][e] : mul_rn(fs[vec[n][e & 1]].x, acc[i][n][e]);
+                  sum[i][n][e] = k == 0 ? mul_rn(e < 2 ? d0 : d1, part) : __fmaf_rn(e < 2 ? d0 : d1, part, sum[i][n][e]);
+                }
             }
           }
 #pragma unroll
           for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const float f = TYPE == LPC_F16 ? 1.f : fs[vec[n][e]];
+              const float f = TYPE == LPC_F16 ? 1.f : fs[vec[n][e]].y;
 #pragma unroll
               for (int i = 0; i < RT; ++i) {
                 tot[i][n][e] = __fmaf_rn(f, sum[i][n][e], tot[i][n][e]);
@@ -819,7 +825,7 @@ cudaError_t launch_forward(const MatvecArgs& a, int vectors, cudaStream_t st) {
   plan.chunk = PD;
   while (plan.chunk * 2 <= cover && plan.chunk < (plan.span + WK - 1) / WK) plan.chunk *= 2;
   while (plan.parts_log2 < 4 && (1 << plan.parts_log2) < plan.span * (4 / LW)) ++plan.parts_log2;
-  const size_t size = 2 * (size_t)plan.chunk * WK * M * (16 * P * 16 + 4) + 2 * 16 * (ROWS + 1) * 4;
+  const size_t size = 2 * (size_t)plan.chunk * WK * M * (16 * P * 16 + (TYPE == LPC_F16 ? 0 : 8)) + 2 * 16 * (ROWS + 1) * 4;
   const size_t smem = std::max(size, (size_t)WK * 8 * NT * ROWS * 4);
   return launch(packed_matvec_kernel<NT, RT, WK, LW, TYPE, NW>, FT, (unsigned)groups, ranks, (unsigned)passes, smem, st, a, plan);
 }
