@@ -264,7 +264,7 @@ int lpc_adamw_state_values(lpc_adamw* h, const void* m, const void* v, const uin
  * X, Y, dX and dY are row-major with row strides ldx, ldy in elements, of one `type` (LPC_F32, LPC_BF16, LPC_F16); sums are held in fp32 and
  * rounded to the type at the end.  Products are exact but for these: a value of X counts to 2^-24 of itself (fp32; the other types exactly) and
  * to 2^-39 of the largest of its 128 columns (fp32 and bf16); dY * delta, rounded to fp32, counts to 2^-18 of itself for the 16-bit
- * types, and as infinite from 3.389e38 on.
+ * types, and to 2^-133.
  * Made for few vectors (M up to some 16: the matrix is read once for all of them);
  * more are taken in turns.  What lies beyond cols or rows in a stride is neither read nor written, and inputs and outputs may not overlap.
  * Sums have a fixed order: the same call gives the same bits.

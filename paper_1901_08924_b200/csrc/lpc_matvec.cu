@@ -488,11 +488,12 @@ template <int TYPE> constexpr int PIECES = TYPE == LPC_F32 ? 3 : 2;
 template <int P>
 __device__ __forceinline__ void split_pair(float x, float y, uint32_t* out) {
   if constexpr (P == 2) {
-    const __nv_bfloat162 hi = __floats2bfloat162_rn(x, y);
-    const uint32_t h = *reinterpret_cast<const uint32_t*>(&hi);
+    // A finite x may round to infinity: the first piece stops at the largest bfloat16 instead, and the second one has the rest.  An infinite x has an
+    // infinite rest.
+    uint32_t h;
+    asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(h) : "f"(y), "f"(x));
     const float fx = __uint_as_float(h << 16), fy = __uint_as_float(h & 0xFFFF0000u);
-    // an infinite x has no rest (NaN); any finite one will do, because the first piece decides the result.  Real ones are above -2^119
-    const __nv_bfloat162 lo = __floats2bfloat162_rn(fmaxf(__fsub_rn(x, fx), -1e37f), fmaxf(__fsub_rn(y, fy), -1e37f));
+    const __nv_bfloat162 lo = __floats2bfloat162_rn(__fsub_rn(x, fx), __fsub_rn(y, fy));
     out[0] = h;
     out[1] = *reinterpret_cast<const uint32_t*>(&lo);
   } else {  // cut off, not rounded: exact, and nothing overflows
