@@ -210,7 +210,7 @@ int lpc_unpack_average_prox(lpc_ctx* ctx, const uint32_t* codes, const float* de
 /*
  * AdamW on the averaged gradient: an adaptive step beside the proximal one, over the tensors of one parameter vector in one launch.  The
  * paper has no counterpart.  For tensor s with lr_s = lr * lr_scale[s], every operation rounded to fp32 (with
- * 8-bit moments the root and the quotient of p' are approximations, within 2^-23 and 2^-22):
+ * 8-bit moments the root and the quotient of p' are approximations, within 2^-23 and 2^-22, and an m' or a quotient below 2^-126 counts as zero there):
  *   g' = g * grad_scale;   m' = beta1 m + (1 - beta1) g';   v' = beta2 v + (1 - beta2) g'^2;
  *   p' = p (1 - lr_s * weight_decay[s]) - lr_s / (1 - beta1^t) * m' / (sqrt(v') / sqrt(1 - beta2^t) + eps).
  * A coordinate whose new moments are not finite numbers below 2^126 (its gradient is NaN or infinite, or its square is) is left as it is,

@@ -42,13 +42,20 @@ constexpr uint32_t MOMENT_LIMIT = 253u << 23;  // 2^126, as bits: moments from h
 
 // The root of the second moment and the quotient of the update.  With 32-bit moments, where memory is what bounds the step, correctly rounded; with 8-bit
 // moments the instructions do, and the hardware's approximations (root: 2^-23 of the value; quotient: 2 units in the last place) take
-// 3 of them where correct rounding takes some 20.  They take numbers below 2^-126 as zeros: next to eps, which is 1e-10 at least, such a second
-// moment's part of the divisor is below half a unit.
+// 3 of them where correct rounding takes some 20.  The root's takes a second moment below 2^-126 as zero, where that is less than half a unit of eps in the
+// divisor: the moment's factor 1 / sqrt(1 - beta2^t) may lift it above that in the first steps of a beta2 next to 1, and those take roots of all
+// floats (3 instructions more, 3 % of the step).  The quotient takes a first moment and a result below 2^-126 as zeros: the divisor is eps, 1e-10, at least, so
+// that they are an update of less than 2^-92 of the step size.
 template <bool APPROXIMATE>
 __device__ __forceinline__ float root(float x) {
   if constexpr (!APPROXIMATE) return __fsqrt_rn(x);
   float r;
   asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float root_of_any(float x) {
+  float r;
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
 template <bool APPROXIMATE>
@@ -228,6 +235,7 @@ __device__ __forceinline__ void add_worker(f32x2* acc, float delta, Word lo, Wor
 struct StepScalars {
   float decay, step, second, gs;
   uint64_t t;
+  bool small_roots;  // 8-bit moments: the root of a second moment below 2^-126 counts next to eps
 };
 
 template <int GRAD, bool BITS8, bool FAST>
@@ -394,7 +402,8 @@ __device__ __forceinline__ void adamw_chunk(const AdamwArgs& a, const StepChunk&
     mul2(p[e], p[e + 1], sc.decay, sc.decay, y[0], y[1]);
     p1[e] = __fsub_rn(y[0], r[0]); p1[e + 1] = __fsub_rn(y[1], r[1]);
   }
-  if (warp_max_u32(max(top_m, top_v)) >= MOMENT_LIMIT) {  // some coordinates stay as they are: what they were is read again
+  const bool beyond = warp_max_u32(max(top_m, top_v)) >= MOMENT_LIMIT;
+  if (beyond || (BITS8 && sc.small_roots)) {  // some coordinates stay as they are, or all weights need another root: what they were is read again
     load8(pj, at, p_at, p);
     if (CODES && !p_at) turn(at, true, p);
     if constexpr (BITS8) {
@@ -410,13 +419,15 @@ __device__ __forceinline__ void adamw_chunk(const AdamwArgs& a, const StepChunk&
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const bool ok = fabsf(m1[e]) < __uint_as_float(MOMENT_LIMIT) && v1[e] < __uint_as_float(MOMENT_LIMIT);
+      if (BITS8 && sc.small_roots)
+        p1[e] = __fsub_rn(mul_rn(p[e], sc.decay), mul_rn(quotient<BITS8>(m1[e], add_rn(mul_rn(root_of_any(v1[e]), sc.second), a.eps)), sc.step));
       m1[e] = ok ? m1[e] : m[e];
       v1[e] = ok ? v1[e] : v[e];
       p1[e] = ok ? p1[e] : p[e];
       top_m = max(top_m, __float_as_uint(m1[e]) & 0x7FFFFFFFu);
       top_v = max(top_v, __float_as_uint(v1[e]) & 0x7FFFFFFFu);
     }
-    if (at.lane == 0) atomicOr(a.dev_status, DEV_NONFINITE);
+    if (beyond && at.lane == 0) atomicOr(a.dev_status, DEV_NONFINITE);
   }
 
   uint16_t h[8];
@@ -472,6 +483,7 @@ __global__ void __launch_bounds__(ST, GRAD >= PACKED && !BITS8 ? 3 : 4) adamw_ke
   sc.decay = __fsub_rn(1.f, mul_rn(lr, c.weight_decay)); sc.step = mul_rn(lr, bc.first); sc.second = bc.second;
   sc.gs = a.grad_scale ? *a.grad_scale : 1.f;
   sc.t = t;
+  sc.small_roots = mul_rn(sc.second, power_of_two(25 - 63)) > a.eps;  // a root below 2^-63 is more than 2^-25 of eps
   // a whole chunk of a tensor that starts on 16 bytes in every array takes code without a thought for anything else
   const int64_t at = c.off + (int64_t)c.chunk * STEP_CHUNK;
   bool fast = (int64_t)(c.chunk + 1) * STEP_CHUNK <= c.len && aligned16(a.p + at) && (!a.copy || aligned16(static_cast<const uint16_t*>(a.copy) + at));
