@@ -239,7 +239,8 @@ int lpc_unpack_average_prox(lpc_ctx* ctx, const uint32_t* codes, const float* de
  * p, g, moments, copy and mu may not overlap.  Beside 16-byte alignment (which is the fast case) p, g, fp32 moments, mu and copy_out
  * may have their element's.
  *
- * lpc_adamw_state_values writes the values of 8-bit moments to m_out and v_out, bf16[len] each (three mantissa bits: exact).
+ * lpc_adamw_state_values writes the values of 8-bit moments to m_out and v_out, bf16[len] each.  They have three mantissa bits and come out exactly; only in a
+ * block whose largest m is below 2^-117, or v below 2^-101, what is below 2^-126 is rounded to the nearest multiple of 2^-133.
  */
 typedef struct lpc_adamw lpc_adamw;
 int lpc_adamw_state_size(int64_t len, const int64_t* seg_offsets, int32_t nseg, int32_t state_bits, int64_t* values_out,

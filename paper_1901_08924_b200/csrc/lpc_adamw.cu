@@ -16,7 +16,7 @@
 // moments and an fp32 gradient (28 bytes a coordinate) 273 us, 6.9 TB/s, memory.  8-bit moments (16 bytes): 196 us, 5.5 TB/s; 72 instructions a coordinate
 // take two thirds of the issue slots.  From 8 workers' 4-bit messages (24 or 12 bytes and 4 of codes): 328 us, 5.7 TB/s, with 32-bit moments, where 80
 // registers leave 24 warps an SM to cover 97 instructions and the loads; 300 us, 3.6 TB/s, with 8-bit ones, 123 instructions in three quarters of the
-// issue slots.  Values of 8-bit moments: 63 us, 6.4 TB/s.  62 tensors of 64 to 2.4 million weights, 11.7 million in all, 32 bits: 54 us (at the copy rate 50).
+// issue slots.  Values of 8-bit moments: 64 us, 6.3 TB/s.  62 tensors of 64 to 2.4 million weights, 11.7 million in all, 32 bits: 54 us (at the copy rate 50).
 // Tensors that start anywhere, 2^25 weights: 152 us (32 bits), 123 us (8 bits).  Slower: five CTAs an SM for 8-bit moments (spills), two chunks a CTA, a loop
 // over chunks that loads the next one while it works on this one.
 #include "lpc_adamw.h"
@@ -495,6 +495,19 @@ __global__ void __launch_bounds__(ST, GRAD >= PACKED && !BITS8 ? 3 : 4) adamw_ke
   else adamw_chunk<GRAD, BITS8, false>(a, c, sc, sdelta, sbuf[tid >> 5]);
 }
 
+// Three mantissa bits: what bfloat16 holds is the upper half of the float.  A block with a small exponent may have steps below 2^-133, where bfloat16 ends; its
+// values, all below 2^-99, are rounded to the nearest multiple of that by a sum whose last place it is.  (By conversions, for all blocks: 65.8 us for 2^26 weights.)
+template <bool SIGNED>
+__device__ __forceinline__ void to_bf16(float* x, uint32_t exponent, uint16_t* h) {
+  if (__builtin_expect(exponent < (SIGNED ? TOP_M : TOP_V) + 2 - 133 + 127, 0)) {
+    const float c = mul_rn(1.5f, power_of_two(23 - 133));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __fsub_rn(add_rn(x[i], c), c);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) h[i] = (uint16_t)(__float_as_uint(x[i]) >> 16);
+}
+
 template <bool FAST>
 __device__ __forceinline__ void values_chunk(const AdamwArgs& a, const StepChunk& c, uint16_t* mo, uint16_t* vo, uint32_t* buf) {
   const int64_t j = (int64_t)c.chunk * STEP_CHUNK + threadIdx.x * 8;
@@ -517,13 +530,11 @@ __device__ __forceinline__ void values_chunk(const AdamwArgs& a, const StepChunk
   float x[8];
   uint16_t h[8];
   decode_moment<true>(cm, e & 0xFFu, x);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) h[i] = (uint16_t)(__float_as_uint(x[i]) >> 16);  // three mantissa bits: nothing is cut off a normal float
+  to_bf16<true>(x, e & 0xFFu, h);
   if (!m_at) turn(at, false, h);
   store8(mo, at, m_at, h);
   decode_moment<false>(cv, e >> 8, x);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) h[i] = (uint16_t)(__float_as_uint(x[i]) >> 16);
+  to_bf16<false>(x, e >> 8, h);
   if (!v_at) turn(at, false, h);
   store8(vo, at, v_at, h);
 }

@@ -64,7 +64,7 @@ struct AdamwArgs {
   unsigned int* dev_status;
 };
 cudaError_t launch_adamw(const AdamwArgs& a, int state_bits, cudaStream_t st);
-// The values of 8-bit moments, in bfloat16 (three mantissa bits: exact).
+// The values of 8-bit moments, in bfloat16 (three mantissa bits: exact where that is a normal number).
 cudaError_t launch_adamw_values(const AdamwArgs& a, void* m_out, void* v_out, cudaStream_t st);
 
 }  // namespace lpc

@@ -489,7 +489,7 @@ class AdamW:
         return p
 
     def state_values(self, state, out=None):
-        """The moments as values: those of 8 bits in bf16 (exact), written to `out` = (m, v) where given; those of 32 bits are themselves."""
+        """The moments as values: those of 8 bits in bf16 (exact but for tiny ones), written to `out` = (m, v) where given; those of 32 bits are themselves."""
         if self.state_bits == 32:
             return state[:2]
         m, v, exps = self._state(state)

@@ -71,3 +71,23 @@ def test_large_gradients_with_8_bit_moments(size, offs):
     for i, which in enumerate("mv"):
         assert (state[i].cpu().numpy() == st[which][0]).all() and (state[2].cpu().numpy()[:, i] == st[which][1]).all()
     opt.close(), ctx.close()
+
+
+@pytest.mark.parametrize("n", [256, 5003])
+def test_values_of_tiny_moments_round_to_the_nearest(n):
+    # every code of blocks with every small exponent: what bfloat16 holds comes out as it is, the rest as its nearest neighbour
+    ctx = base._ctx()
+    opt = lpc.AdamW(ctx, n, None, 8)
+    blocks = -(-n // 256)
+    every = np.tile(np.arange(256, dtype=np.uint8), blocks)
+    codes = {"m": every, "v": every}
+    for first in list(range(1, 60, blocks)) + [100, 127, 200]:
+        e = (first + np.arange(blocks)).astype(np.uint8)
+        exps = np.stack([e, e], 1)
+        got = opt.state_values((base._dev(codes["m"]), base._dev(codes["v"]), base._dev(exps)))
+        ctx.sync_status()
+        for x, which in zip(got, "mv"):
+            value = lb.decode(which, codes[which].reshape(-1, 256), e).ravel()[:n]
+            want = torch.from_numpy(value).float().bfloat16()   # no code is near a tie that the first rounding could move: both keep to even
+            assert torch.equal(x.cpu(), want), (first, which)
+    opt.close(), ctx.close()
