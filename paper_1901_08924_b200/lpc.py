@@ -155,7 +155,8 @@ def packed_layout(length, b, seg_offsets=None):
 
 class Context:
     """Owns one lpc_ctx.  X and y are CUDA fp32 tensors kept alive by this object (or None for a
-    quantizer-only context)."""
+    quantizer-only context).  All work goes to `stream` (torch's current one where none is given) and is in order with that alone: what was written on another
+    stream has to be ready before a call, and results are used on another one behind an event or sync_status."""
 
     def __init__(self, X, y, loss, lambda_l1, N, B, b, clip_mode, clip_value, seed, stream=None):
         self._h = C.c_void_p(None)
@@ -171,6 +172,7 @@ class Context:
         self._device_index = self.device.index
         self.n, self.d, self.N, self.B, self.b = n, d, N, B, b
         self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
+        self._raw_stream = self.stream.cuda_stream
         self._lib = lib()
         self._layouts = {}  # (length, bits) -> (seg_offsets, C array, segments, stride in words) of the last call
         rc = lib().lpc_init(C.byref(self._h), _ptr(X), _ptr(y), n, d, loss, lambda_l1, N, B, b, clip_mode, clip_value,
@@ -184,6 +186,17 @@ class Context:
     def _ck(self, rc):
         if rc != OK:
             raise LpcError(rc, lib().lpc_last_error(self._h).decode())
+
+    def _new(self, shape, dtype):
+        """Memory for a result.  The context's stream writes it, so where that is not torch's current one it comes from what the allocator keeps for the
+        context's stream: the current stream may still have work queued on a block that it gave back."""
+        if torch._C._cuda_getCurrentRawStream(self._device_index) == self._raw_stream:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        current = torch.cuda.current_stream(self.device)
+        with torch.cuda.stream(self.stream):
+            t = torch.empty(shape, dtype=dtype, device=self.device)
+        t.record_stream(current)  # where the caller will use it, once the two streams are in step
+        return t
 
     def _layout(self, length, bits, seg_offsets):
         """C array of the offsets, segment count and stride in words; the last layout of a width is kept, because a training
@@ -229,7 +242,7 @@ class Context:
                 BUF_BATCH_IDX: (N + 1, B), BUF_COEF: (N + 1, B), BUF_U: (N, d)}.get(which, (d,))
 
     def get_buffer(self, which):
-        t = torch.empty(self._buf_shape(which), dtype=self._BUF_DTYPE.get(which, torch.float32), device=self.device)
+        t = self._new(self._buf_shape(which), self._BUF_DTYPE.get(which, torch.float32))
         self._ck(lib().lpc_get_buffer(self._h, which, _ptr(t), t.numel() * t.element_size()))
         return t
 
@@ -242,7 +255,7 @@ class Context:
         self._ck(lib().lpc_set_iterate(self._h, _ptr(x)))
 
     def get_iterate(self):
-        x = torch.empty(self.d, dtype=torch.float32, device=self.device)
+        x = self._new(self.d, torch.float32)
         self._ck(lib().lpc_get_iterate(self._h, _ptr(x)))
         return x
 
@@ -267,11 +280,11 @@ class Context:
             assert U_sub.shape == shape and U_sub.stride() == strides and U_sub.dtype == torch.float32
         arr, nseg, stride = self._layout(length, self.b, seg_offsets)
         if codes_out is None:
-            codes_out = torch.empty((self.N, stride), dtype=torch.int32, device=U.device)
+            codes_out = self._new((self.N, stride), torch.int32)
         if delta_out is None:
-            delta_out = torch.empty((self.N, nseg), dtype=torch.float32, device=U.device)
+            delta_out = self._new((self.N, nseg), torch.float32)
         if clipped_out is None:
-            clipped_out = torch.empty((self.N, nseg), dtype=torch.int32, device=U.device)
+            clipped_out = self._new((self.N, nseg), torch.int32)
         rc = self._lib.lpc_quantize_pack(self._h, U.data_ptr(), _ptr(U_sub), length, ld, arr, nseg, k, codes_out.data_ptr(),
                                          delta_out.data_ptr(), clipped_out.data_ptr())
         if rc != OK:
@@ -291,7 +304,7 @@ class Context:
         Returns (hist (N, nseg, 2^b) int64 CUDA tensor, entropy (N, nseg) or None, huffman (N, nseg) or None)."""
         arr, nseg, _ = self._layout(length, self.b, seg_offsets)
         if hist_out is None:
-            hist_out = torch.empty((self.N, nseg, 1 << self.b), dtype=torch.int64, device=codes.device)
+            hist_out = self._new((self.N, nseg, 1 << self.b), torch.int64)
         if not host_counts:
             self._ck(self._lib.lpc_message_entropy(self._h, _ptr(codes), length, arr, nseg, _ptr(hist_out), None, None))
             return hist_out, None, None
@@ -305,7 +318,7 @@ class Context:
         bo = sum_bits(self.b, self.N) if scheme == SCHEME_SERVER_SUM else self.b
         arr, nseg, stride = self._layout(length, bo, seg_offsets)
         if codes_out is None:
-            codes_out = torch.empty((1, stride), dtype=torch.int32, device=codes.device)
+            codes_out = self._new((1, stride), torch.int32)
         self._ck(lib().lpc_server_reduce(self._h, _ptr(codes), length, arr, nseg, scheme, k, _ptr(codes_out)))
         return codes_out, bo
 
@@ -328,7 +341,7 @@ class Context:
         assert delta.shape == (rows, -(-cols // group) if group else min(cols, 1))
         assert x.get_device() == self._device_index and dtype in _TYPES and have == need and (have <= 1 or ld[1] == 1)
         if out is None:
-            out, ldo = x.new_empty((M, want)), want
+            out, ldo = self._new((M, want), dtype), want
         else:
             ldo = out.stride()
             assert out.get_device() == self._device_index and out.dtype is dtype and out.shape == (M, want) and (want <= 1 or ldo[1] == 1)
@@ -431,12 +444,20 @@ class AdamW:
             pass
 
     def init_state(self, device=None):
-        """Moments before the first step: zeros."""
-        device = device or self.ctx.device
-        if self.state_bits == 32:
-            return tuple(torch.zeros(self.length, dtype=torch.float32, device=device) for _ in range(2)) + (None,)
-        return tuple(torch.zeros(self.state_values_count, dtype=torch.uint8, device=device) for _ in range(2)) + (
-            torch.zeros(self.state_exps_count, dtype=torch.uint8, device=device).view(-1, 2),)
+        """Moments before the first step: zeros, which the context's stream writes and torch's current one waits for."""
+        values = (self.length, torch.float32) if self.state_bits == 32 else (self.state_values_count, torch.uint8)
+        shapes = [values, values] + ([(self.state_exps_count, torch.uint8)] if self.state_bits == 8 else [])
+        if device is not None:
+            m, v, *exps = [torch.zeros(n, dtype=dtype, device=device) for n, dtype in shapes]
+        else:
+            m, v, *exps = [self.ctx._new(n, dtype) for n, dtype in shapes]
+            with torch.cuda.stream(self.ctx.stream):
+                for t in (m, v, *exps):
+                    t.zero_()
+            current = torch.cuda.current_stream(self.ctx.device)
+            if current != self.ctx.stream:
+                current.wait_stream(self.ctx.stream)
+        return m, v, exps[0].view(-1, 2) if exps else None
 
     def _state(self, state):
         m, v, exps = state
@@ -494,7 +515,7 @@ class AdamW:
             return state[:2]
         m, v, exps = self._state(state)
         if out is None:
-            out = tuple(torch.empty(self.length, dtype=torch.bfloat16, device=state[0].device) for _ in range(2))
+            out = tuple(self.ctx._new(self.length, torch.bfloat16) for _ in range(2))
         assert all(o.get_device() == self._device_index and o.dtype is torch.bfloat16 and o.numel() == self.length and o.is_contiguous() for o in out)
         rc = self._lib.lpc_adamw_state_values(self._open(), m, v, exps, out[0].data_ptr(), out[1].data_ptr())
         if rc != OK:
