@@ -111,6 +111,11 @@ def _ptr(t):  # a c_void_p argument also takes the plain integer
     return None if t is None else t.data_ptr()
 
 
+def _records(*tensors):
+    """Whether autograd would record a call that takes these."""
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+
+
 def _seg(seg_offsets):
     if seg_offsets is None:
         return None, 1
@@ -324,7 +329,8 @@ class Context:
 
     def packed_matvec(self, codes, delta, cols, X, group=128, out=None):
         """Y = X W^T with W in packed 4-bit rows: codes (rows, stride) int32, delta (rows, groups) fp32 as quantize_pack writes them for
-        segments of `group` columns (0: one scale per row).  X (M, cols) fp32, bf16 or fp16; returns Y (M, rows) of the same type."""
+        segments of `group` columns (0: one scale per row).  X (M, cols) fp32, bf16 or fp16; returns Y (M, rows) of the same type.  Nothing is
+        recorded for autograd, so an X that requires grad is refused: detach it, packed_matvec_t is its gradient."""
         return self._packed_product(self._lib.lpc_packed_matvec, codes, delta, cols, X, group, out, False)
 
     def packed_matvec_t(self, codes, delta, cols, dY, group=128, out=None):
@@ -340,6 +346,7 @@ class Context:
         assert delta.get_device() == self._device_index and delta.dtype is torch.float32 and delta.is_contiguous()
         assert delta.shape == (rows, -(-cols // group) if group else min(cols, 1))
         assert x.get_device() == self._device_index and dtype in _TYPES and have == need and (have <= 1 or ld[1] == 1)
+        assert not _records(x, delta, out), "products with packed rows are not recorded for autograd: detach their arguments (packed_matvec_t is the gradient for X)"
         if out is None:
             out, ldo = self._new((M, want), dtype), want
         else:
