@@ -111,9 +111,9 @@ def _ptr(t):  # a c_void_p argument also takes the plain integer
     return None if t is None else t.data_ptr()
 
 
-def _records(*tensors):
-    """Whether autograd would record a call that takes these."""
-    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+# Tells autograd that the library wrote a tuple of tensors: a backward pass that saved one of them refuses to run, as behind any operation in place.
+_written = torch._C._increment_version
+_current_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
 def _seg(seg_offsets):
@@ -195,7 +195,7 @@ class Context:
     def _new(self, shape, dtype):
         """Memory for a result.  The context's stream writes it, so where that is not torch's current one it comes from what the allocator keeps for the
         context's stream: the current stream may still have work queued on a block that it gave back."""
-        if torch._C._cuda_getCurrentRawStream(self._device_index) == self._raw_stream:
+        if _current_raw_stream(self._device_index) == self._raw_stream:
             return torch.empty(shape, dtype=dtype, device=self.device)
         current = torch.cuda.current_stream(self.device)
         with torch.cuda.stream(self.stream):
@@ -346,9 +346,11 @@ class Context:
         assert delta.get_device() == self._device_index and delta.dtype is torch.float32 and delta.is_contiguous()
         assert delta.shape == (rows, -(-cols // group) if group else min(cols, 1))
         assert x.get_device() == self._device_index and dtype in _TYPES and have == need and (have <= 1 or ld[1] == 1)
-        assert not _records(x, delta, out), "products with packed rows are not recorded for autograd: detach their arguments (packed_matvec_t is the gradient for X)"
-        if out is None:
-            out, ldo = self._new((M, want), dtype), want
+        assert not (torch.is_grad_enabled() and (x.requires_grad or delta.requires_grad or (out is not None and out.requires_grad))), "products with packed rows are not recorded for autograd: detach their arguments (packed_matvec_t is the gradient for X)"
+        given = out is not None
+        if not given:
+            out = x.new_empty((M, want)) if _current_raw_stream(self._device_index) == self._raw_stream else self._new((M, want), dtype)
+            ldo = want
         else:
             ldo = out.stride()
             assert out.get_device() == self._device_index and out.dtype is dtype and out.shape == (M, want) and (want <= 1 or ldo[1] == 1)
@@ -357,6 +359,8 @@ class Context:
                 ld[0] if M > 1 else have, out.data_ptr(), ldo)
         if rc != OK:
             self._ck(rc)
+        if given:
+            _written((out,))
         return out
 
     def set_strong_convexity(self, sigma):
@@ -479,6 +483,8 @@ class AdamW:
 
     def _scalars(self, t, lr_dev, t_dev, grad_scale, copy_out):
         assert t >= 0  # the C argument has no sign
+        if lr_dev is t_dev is grad_scale is copy_out is None:
+            return None, None, None, None, BF16
         for s, dtype in ((lr_dev, torch.float32), (t_dev, torch.int64), (grad_scale, torch.float32)):
             assert s is None or (s.get_device() == self._device_index and s.dtype is dtype and s.numel() == 1)
         if copy_out is None:
@@ -494,6 +500,12 @@ class AdamW:
         assert p.get_device() == self._device_index and p.dtype is torch.float32 and p.numel() == self.length and p.is_contiguous()
         return p.data_ptr()
 
+    def _mark(self, p, state, copy_out):
+        m, v, exps = state
+        _written((p, m, v, exps) if self.state_bits == 8 else (p, m, v))
+        if copy_out is not None:
+            _written((copy_out,))
+
     def step(self, p, g, state, t, lr, lr_dev=None, t_dev=None, grad_scale=None, copy_out=None):
         """One step, number t (from 1), with the gradient g: fp32, bf16 or fp16."""
         assert g.get_device() == self._device_index and g.dtype in _TYPES and g.numel() == self.length and g.is_contiguous()
@@ -501,6 +513,7 @@ class AdamW:
                                       *self._scalars(t, lr_dev, t_dev, grad_scale, copy_out))
         if rc != OK:
             self.ctx._ck(rc)
+        self._mark(p, state, copy_out)
         return p
 
     def unpack_average_step(self, codes, delta, p, state, t, lr, mu=None, lr_dev=None, t_dev=None, grad_scale=None, copy_out=None):
@@ -514,6 +527,7 @@ class AdamW:
                                                 *self._state(state), t, lr, *self._scalars(t, lr_dev, t_dev, grad_scale, copy_out))
         if rc != OK:
             self.ctx._ck(rc)
+        self._mark(p, state, copy_out)
         return p
 
     def state_values(self, state, out=None):
@@ -527,6 +541,7 @@ class AdamW:
         rc = self._lib.lpc_adamw_state_values(self._open(), m, v, exps, out[0].data_ptr(), out[1].data_ptr())
         if rc != OK:
             self.ctx._ck(rc)
+        _written(out)
         return out
 
 
