@@ -222,7 +222,7 @@ int lpc_unpack_average_prox(lpc_ctx* ctx, const uint32_t* codes, const float* de
  *   state_bits   32: m and v are fp32[len], laid out like p.  8: m and v are bytes, lpc_adamw_state_size says how many (16-byte
  *                aligned), and exps holds two bytes a block of 256 coordinates of a tensor (2-byte aligned).  Zeroed memory is the
  *                state before the first step either way.
- *   eps > 0 (with 8-bit moments >= 1e-10), 0 <= beta < 1;  weight_decay, lr_scale: host, nseg values >= 0, nullable (0 and 1)
+ *   eps > 0 (with 8-bit moments 1e-10 to 2^125), 0 <= beta < 1;  weight_decay, lr_scale: host, nseg values >= 0, nullable (0 and 1)
  * Moments in 8 bits are floats with 3 mantissa bits, m with a sign and 4 exponent bits, v with 5 and no sign, relative to the largest
  * power of two of the block, rounded stochastically (unbiased, like rule (1) of Section 2.2; a nonzero v never to zero) with the
  * context's seed: coordinate j of the padded blocks uses 16-bit lane j%8 of block j/8 of stream (tag 5 for m, 6 for v; worker 0, k = t).

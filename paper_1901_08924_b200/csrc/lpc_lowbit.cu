@@ -123,7 +123,9 @@ int lpc_adamw_create(lpc_adamw** out, lpc_ctx* ctx, int64_t len, const int64_t* 
   if (state_bits != 8 && state_bits != 32) return ctx_fail(ctx, LPC_ERR_INVALID_ARG, "moments have 8 or 32 bits");
   if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0)) return ctx_fail(ctx, LPC_ERR_INVALID_ARG, "beta1 and beta2 are in [0, 1)");
   if (!((float)beta1 < 1.f) || !((float)beta2 < 1.f)) return ctx_fail(ctx, LPC_ERR_INVALID_ARG, "beta1 or beta2 rounds to 1");
-  if (!(eps > 0.f) || !std::isfinite(eps) || (state_bits == 8 && eps < 1e-10f)) return ctx_fail(ctx, LPC_ERR_INVALID_ARG, "eps is above 0, with 8-bit moments at least 1e-10");
+  // with 8-bit moments the quotient's approximation gives 0 for divisors above 2^126
+  if (!(eps > 0.f) || !std::isfinite(eps) || (state_bits == 8 && !(eps >= 1e-10f && eps <= 0x1p125f)))
+    return ctx_fail(ctx, LPC_ERR_INVALID_ARG, "eps is above 0, with 8-bit moments from 1e-10 to 2^125");
   for (int s = 0; s < nseg; ++s) {
     if (weight_decay && !(weight_decay[s] >= 0.f && std::isfinite(weight_decay[s]))) return ctx_fail(ctx, LPC_ERR_INVALID_ARG, "weight decay");
     if (lr_scale && !(lr_scale[s] >= 0.f && std::isfinite(lr_scale[s]))) return ctx_fail(ctx, LPC_ERR_INVALID_ARG, "lr scale");

@@ -91,3 +91,21 @@ def test_values_of_tiny_moments_round_to_the_nearest(n):
             want = torch.from_numpy(value).float().bfloat16()   # no code is near a tie that the first rounding could move: both keep to even
             assert torch.equal(x.cpu(), want), (first, which)
     opt.close(), ctx.close()
+
+
+def test_an_eps_that_the_approximate_quotient_cannot_divide_by_is_refused():
+    n = 512
+    ctx = base._ctx()
+    for eps in (2.0 ** 126, 2.0 ** 127):
+        with pytest.raises(lpc.LpcError) as e:
+            lpc.AdamW(ctx, n, None, 8, (0.9, 0.999), eps)
+        assert e.value.code == lpc.ERR_INVALID_ARG
+    for bits, eps in ((8, 2.0 ** 125), (32, 2.0 ** 127)):
+        # beta1 = 0 and a gradient of 2^60: the update is 2^60 / (eps + 2^60), far below eps
+        opt = lpc.AdamW(ctx, n, None, bits, (0.0, 0.999), eps)
+        p = torch.zeros(n, device=DEV)
+        opt.step(p, torch.full((n,), 2.0 ** 60, device=DEV), opt.init_state(), 1, 1.0)
+        ctx.sync_status()
+        assert ((p.double() * eps / 2.0 ** 60 + 1).abs() <= 2.0 ** -20).all()
+        opt.close()
+    ctx.close()
