@@ -293,26 +293,24 @@ __device__ __forceinline__ void adamw_chunk(const AdamwArgs& a, const StepChunk&
         if (first + i < a.N) fetch(first + i, l[i], h[i]);
     }
   };
-  if (at.count > 0) {
-    load8(pj, at, p_at, p);
-    if constexpr (BITS8) {
-      if (at.n > 0) {
-        cm = *reinterpret_cast<const uint2*>(m8);
-        cv = *reinterpret_cast<const uint2*>(v8);
-      }
-      exps = reinterpret_cast<const uint16_t*>(a.exps)[block];
-    } else {
-      load8(m32, at, m_at, m);
-      load8(v32, at, v_at, v);
+  load8(pj, at, p_at, p);
+  if constexpr (BITS8) {
+    if (at.n > 0) {
+      cm = *reinterpret_cast<const uint2*>(m8);
+      cv = *reinterpret_cast<const uint2*>(v8);
     }
-    if constexpr (GRAD == LPC_F32) load8(gj, at, g_at, g);
-    else if constexpr (GRAD < PACKED) load8(ghj, at, g_at, gh);
-    else {
-      if constexpr (BITS != 32) {
-        if (at.n > 0) fetch_group(0, lo, hi);
-      }
-      if (a.mu) load8(muj, at, mu_at, mu);
+    exps = reinterpret_cast<const uint16_t*>(a.exps)[block];
+  } else {
+    load8(m32, at, m_at, m);
+    load8(v32, at, v_at, v);
+  }
+  if constexpr (GRAD == LPC_F32) load8(gj, at, g_at, g);
+  else if constexpr (GRAD < PACKED) load8(ghj, at, g_at, gh);
+  else {
+    if constexpr (BITS != 32) {
+      if (at.n > 0) fetch_group(0, lo, hi);
     }
+    if (a.mu) load8(muj, at, mu_at, mu);
   }
   if constexpr (CODES) {
     if (!p_at) turn(at, true, p);

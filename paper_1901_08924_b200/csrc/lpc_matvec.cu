@@ -31,9 +31,6 @@ constexpr int SLAB = 128;  // columns of codes that a quad takes at a time: 16 w
 __device__ __forceinline__ float half_value(uint32_t h, int type) {
   return type == LPC_BF16 ? __uint_as_float(h << 16) : __half2float(__ushort_as_half((unsigned short)h));
 }
-__device__ __forceinline__ float value_of(const void* p, int64_t i, int type) {
-  return type == LPC_F32 ? static_cast<const float*>(p)[i] : half_value(static_cast<const uint16_t*>(p)[i], type);
-}
 __device__ __forceinline__ void store_value(void* p, int64_t i, int type, float v) {
   if (type == LPC_F32) static_cast<float*>(p)[i] = v;
   else if (type == LPC_BF16) static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
