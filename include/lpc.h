@@ -15,7 +15,8 @@
  *    The library never frees or reallocates them.  They must be 16-byte aligned, fp32 data must
  *    be finite.  X is row-major, contiguous, leading dimension d, and d must be a multiple of 4.
  *  - Work is enqueued on the cudaStream_t given to lpc_init (passed as void*); calls return
- *    without waiting unless they hand back a host scalar (said per call).  Device-side problems
+ *    without waiting unless they hand back a host scalar (said per call).  Nothing is ordered with
+ *    other streams: arrays must be ready on this one, and results are used behind it.  Device-side problems
  *    (non-finite input, a bounded wait that ran out) are recorded in the context and reported by
  *    the next lpc_sync_status().
  *  - A context may be used by one host thread at a time.
@@ -214,11 +215,13 @@ int lpc_unpack_average_prox(lpc_ctx* ctx, const uint32_t* codes, const float* de
  *   g' = g * grad_scale;   m' = beta1 m + (1 - beta1) g';   v' = beta2 v + (1 - beta2) g'^2;
  *   p' = p (1 - lr_s * weight_decay[s]) - lr_s / (1 - beta1^t) * m' / (sqrt(v') / sqrt(1 - beta2^t) + eps).
  * A coordinate whose new moments are not finite numbers below 2^126 (its gradient is NaN or infinite, or its square is) is left as it is,
- * moments and weight, and lpc_sync_status then returns LPC_ERR_NONFINITE.
+ * moments and weight, and lpc_sync_status then returns LPC_ERR_NONFINITE.  (8-bit moments stay as the values they stand for: where the block's largest
+ * power of two changes they are rounded to its new grid like the others.)
  *
  * lpc_adamw_create makes a handle for vectors of `len` values in nseg tensors (seg_offsets as in lpc_packed_layout, any offsets, tensors of
  * length 0 included; offsets that are multiples of 8 are the fast ones).  It holds the table of the tensors on the context's device, nothing
- * of the caller's; it works on the context's stream and must be destroyed before the context.  Make it outside stream captures.
+ * of the caller's; it works on the context's stream and must be destroyed before the context.  Make it outside stream captures; a
+ * graph of its calls reads the table, so destroy it behind the last replay.
  *   state_bits   32: m and v are fp32[len], laid out like p.  8: m and v are bytes, lpc_adamw_state_size says how many (16-byte
  *                aligned), and exps holds two bytes a block of 256 coordinates of a tensor (2-byte aligned).  Zeroed memory is the
  *                state before the first step either way.
@@ -226,6 +229,8 @@ int lpc_unpack_average_prox(lpc_ctx* ctx, const uint32_t* codes, const float* de
  * Moments in 8 bits are floats with 3 mantissa bits, m with a sign and 4 exponent bits, v with 5 and no sign, relative to the largest
  * power of two of the block, rounded stochastically (unbiased, like rule (1) of Section 2.2; a nonzero v never to zero) with the
  * context's seed: coordinate j of the padded blocks uses 16-bit lane j%8 of block j/8 of stream (tag 5 for m, 6 for v; worker 0, k = t).
+ * Handles of one context round with the same random numbers at the same t: where that matters (parameter groups of a handle each) make them on contexts of
+ * different seeds, or one handle with lr_scale and weight_decay for each tensor.
  * The sum of all tensors' padded lengths must be below 2^35.
  *
  * lpc_adamw_step takes a dense gradient g (fp32, bf16 or fp16).  lpc_unpack_average_adamw takes the N workers' packed messages (codes
@@ -260,13 +265,15 @@ int lpc_adamw_state_values(lpc_adamw* h, const void* m, const void* v, const uin
  * for `rows` vectors of `cols` values whose segments are groups of `group` columns (the last one shorter) -- row r's codes start at
  * word r * stride_words, stride_words = ceil(cols / 32) * 4, its scales at delta[r * groups].  The paper has no counterpart: a worker uses the
  * weights it was sent as codes, without unpacking them to memory.
+ * A context has at most 1,024 workers: a matrix of more rows takes a call of lpc_quantize_pack for each 1,024 of them into their part of one array of codes and
+ * one of scales, with a k of its own each time (workers of equal number share their rounding variables), and one on a context of fewer workers for the rest.
  *   lpc_packed_matvec     Y[m][r] = sum_k X[m][k] W[r][k],  m < M
  *   lpc_packed_matvec_t   dX[m][k] = sum_r dY[m][r] W[r][k]: the gradient of the first for X
  * X, Y, dX and dY are row-major with row strides ldx, ldy in elements, of one `type` (LPC_F32, LPC_BF16, LPC_F16); sums are held in fp32 and
- * rounded to the type at the end.  Products are exact but for these: a value of X counts to 2^-24 of itself (fp32; the other types exactly) and
+ * rounded to the type at the end.  Products are exact but for these: a value of X counts to 2^-23 of itself (fp32; the other types exactly) and
  * to 2^-39 of the largest of its 128 columns (fp32 and bf16); dY * delta, rounded to fp32, counts to 2^-18 of itself for the 16-bit
  * types, and to 2^-133.
- * Made for few vectors (M up to some 16: the matrix is read once for all of them);
+ * Made for few vectors: the matrix is read once for up to 32 of them (fp32: 16), transposed for up to 16 (fp32: 8);
  * more are taken in turns.  What lies beyond cols or rows in a stride is neither read nor written, and inputs and outputs may not overlap.
  * Sums have a fixed order: the same call gives the same bits.
  *   group   a multiple of 32 columns, or 0: one scale per row

@@ -142,7 +142,7 @@ struct MatvecPlan {
 //
 // The vectors are fp16 pieces.  An fp16 vector is its own piece.  128 columns of another are multiplied by the power of two that brings their
 // largest magnitude to 2^14 .. 2^15, which the sums are divided by again; a bfloat16 vector (8 significant bits) is then one piece, an fp32
-// vector two (11 bits each and the sign of the second: 2^-24 of a value is lost, half a step of fp32).  What falls out of fp16's
+// vector two (11 bits each and the sign of the second: of 24 bits the last may be lost, 2^-23 of a value at most).  What falls out of fp16's
 // range at the lower end is below 2^-39 of the largest of the 128.  Where one of the 128 is not finite, every product with them is
 // infinite or NaN whatever the others are: those are taken as zeros, so that none of them overflows.
 // Small vectors are multiplied by much, and a sum of 128 products, up to 2^25 then, times a large scale could leave the floats though the result does not:
