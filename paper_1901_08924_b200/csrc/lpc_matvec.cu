@@ -765,8 +765,8 @@ __global__ void __launch_bounds__(MT, PIECES<TYPE> * MP <= 16 ? 2 : 1) packed_ma
 
 template <class Kernel>
 cudaError_t launch(Kernel kernel, int threads, unsigned groups, int ranks, unsigned passes, size_t smem, cudaStream_t st, const MatvecArgs& a, const MatvecPlan& plan) {
-  if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (smem > 48 * 1024) {  // always up to all there is: another host thread, whose call takes less, must not lower it before this launch
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
     if (e != cudaSuccess) return e;
   }
   cudaLaunchConfig_t cfg = {};
