@@ -16,7 +16,8 @@
  *    be finite.  X is row-major, contiguous, leading dimension d, and d must be a multiple of 4.
  *  - Work is enqueued on the cudaStream_t given to lpc_init (passed as void*); calls return
  *    without waiting unless they hand back a host scalar (said per call).  Nothing is ordered with
- *    other streams: arrays must be ready on this one, and results are used behind it.  Device-side problems
+ *    other streams: arrays must be ready on this one and stay until it has passed the call, and
+ *    results are used behind it.  Device-side problems
  *    (non-finite input, a bounded wait that ran out) are recorded in the context and reported by
  *    the next lpc_sync_status().
  *  - A context may be used by one host thread at a time.
