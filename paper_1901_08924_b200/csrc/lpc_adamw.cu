@@ -15,10 +15,11 @@
 // What bounds it.  One pass, eight consecutive coordinates a thread, everything asked for before anything is waited for.  2^26 weights: with 32-bit
 // moments and an fp32 gradient (28 bytes a coordinate) 273 us, 6.9 TB/s, memory.  8-bit moments (16 bytes): 196 us, 5.5 TB/s; 72 instructions a coordinate
 // take two thirds of the issue slots.  From 8 workers' 4-bit messages (24 or 12 bytes and 4 of codes): 328 us, 5.7 TB/s, with 32-bit moments, where 80
-// registers leave 24 warps an SM to cover 97 instructions and the loads; 300 us, 3.6 TB/s, with 8-bit ones, 123 instructions in three quarters of the
+// registers leave 24 warps an SM to cover 86 instructions and the loads; 300 us, 3.6 TB/s, with 8-bit ones, 109 instructions in two thirds of the
 // issue slots.  Values of 8-bit moments: 64 us, 6.3 TB/s.  62 tensors of 64 to 2.4 million weights, 11.7 million in all, 32 bits: 54 us (at the copy rate 50).
-// Tensors that start anywhere, 2^25 weights: 152 us (32 bits), 123 us (8 bits).  Slower: five CTAs an SM for 8-bit moments (spills), two chunks a CTA, a loop
-// over chunks that loads the next one while it works on this one.
+// Tensors that start anywhere, 2^25 weights: 152 us (32 bits), 124 us (8 bits).  Slower: five CTAs an SM for 8-bit moments (more spills), two chunks a CTA, a loop
+// over chunks that loads the next one while it works on this one.  2^24 weights from 8 workers' messages: 84 to 94 us for 1, 2, 3, 4 and 8 bits (32-bit moments) and 73 to
+// 94 (8-bit); widths known at run time 151 (16 bits) to 241 us (12 bits), 142 to 199.  All instances spill, those of 8 bits and run-time widths 400 to 580 bytes a thread.
 #include "lpc_adamw.h"
 
 #include <cuda_bf16.h>

@@ -136,8 +136,8 @@ struct MatvecPlan {
 // operands of 8 RT matrix instructions; which of the slab's columns sit at which place of the instruction's contraction is free as long as
 // the vectors, laid out in shared memory, follow the same order.  LW: consecutive words a lane takes of a row, chosen so that an
 // instruction never mixes groups of columns with different scales: 32 LW columns make up a group or a part of one.  WK warps share the rows'
-// columns, and CTAs of a cluster do (through distributed shared memory at the end, without a workspace), so that few rows fill the
-// chip; 8 / WK have rows of their own, so that the vectors, which every CTA lays out for itself, are not laid out too often.  Codes
+// columns, and CTAs of a cluster do (through distributed shared memory at the end, without a workspace), so that some thousand rows fill the
+// chip (eight CTAs at most share theirs: 128 rows leave 140 SMs idle); 8 / WK have rows of their own, so that the vectors, which every CTA lays out for itself, are not laid out too often.  Codes
 // go from memory to the registers they are used in, AHEAD slabs before (copies to shared memory and more slabs ahead were no gain).
 //
 // The vectors are fp16 pieces.  An fp16 vector is its own piece.  128 columns of another are multiplied by the power of two that brings their
@@ -150,9 +150,8 @@ struct MatvecPlan {
 // 1 the first product is below the scale and the second one smaller still; where it is not, what overflows does so rightly.
 //
 // 16384 x 16384, groups of 128: 33 us for one vector (4.3 TB/s; 24 us with nothing to read, 28 us with a quarter of the arithmetic: both sides
-// overlap, but not fully with the 16 warps an SM that the registers allow), 43 us for 8, 57 us for 16, where laying out the
-// vectors and the matrix instructions' operands take most; groups of 32, one vector: 64 us.  4096 x 4096, one vector: 5.9 us, of which a
-// launch is 3.
+// overlap, but not fully with the 16 warps an SM that the registers allow), 44 us for 8, 58 us for 16 (a third of the instructions unpack, 0.4 of 3.5 a code scale), 119 us
+// for 16 in fp32; groups of 32, one vector: 64 us (floors 21.8 to 25.6).  4096 x 4096, one vector: 6.1 us, of which a launch is 3.
 template <int NT, int LW> constexpr int AHEAD = LW == 4 && NT < 4 ? 2 : 1;  // slabs of codes on their way
 // Eights of columns that a thread brings in at a time: those of AHEAD turns of all the vectors of a pass, or more.
 template <int NT, int WK, int LW, int NW> constexpr int TASKS_OF = (AHEAD<NT, LW> * WK * 16 * 8 * NT + NW * 32 - 1) / (NW * 32);
@@ -469,10 +468,10 @@ __global__ void __launch_bounds__(NW * 32, 16 / NW) packed_matvec_kernel(MatvecA
 // two pieces, for outputs of 8 or 11 significant bits, 2^-18 of a factor is lost; three hold all of it.
 // WC blocks of 128 columns make up a CTA, and 8 / WC warps share a block's rows.  Scales of 512 rows at a time are copied to shared memory: a row's are
 // next to each other and far from the next row's, so that every lane fetching its own kept the memory pipe busy with single words (16384 x 8192, groups of
-// 64, 8 vectors: 53 us, 35 us of them with no scales to fetch).  At 16384 x 16384 one vector takes 56 us, 16 take 105 and 16 fp32 ones 178; with 256 rows,
-// through registers, 59, 129 and 228; with 1024 rows groups of 32 take 80 us instead of 74.
-// 16384 x 8192, groups of 64, 8 vectors: 38 us (floor 11.6); 16384 x 16384, groups of 128, one vector: 56 us (floor 21.8), of which some 40 pass with the
-// codes at hand: the operands' instructions, more than three a code, bound it.  4096 x 4096, one vector: 8.3 us, of which a launch is 3.
+// 64, 8 vectors: 53 us, 35 us of them with no scales to fetch).  At 16384 x 16384 one vector takes 55 us, 16 take 103 and 16 fp32 ones 178; with 256 rows,
+// through registers, 59, 129 and 228; with 1024 rows groups of 32 took 80 us instead of 74 (now 71).
+// 16384 x 8192, groups of 64, 8 vectors: 36 us (floor 11.6); 16384 x 16384, groups of 128, one vector: 55 us (floor 21.8), of which some 40 pass with the
+// codes at hand: the operands' instructions, 3.5 a code, bound it.  4096 x 4096, one vector: 8.3 us, of which a launch is 3.
 constexpr int SCALE_ROWS = 512;
 // Codes are copied to shared memory RING - 1 steps ahead, a lane's words 2g and 2g + 1 of its four rows (groups of 32, where a lane has half words of
 // its rows to fetch: 95 us -> 74 us for one vector at 16384 x 16384; 8 slots took 2 % longer than 4).  TROW and the place of a quad's rows keep banks
