@@ -84,3 +84,46 @@ def test_the_current_streams_own_work_on_new_moments_comes_behind_their_zeros():
     torch.cuda.synchronize()
     assert (m == 3).all() and (v == 0).all()
     opt.close(), ctx.close()
+
+
+def test_a_capture_that_forks_to_the_contexts_stream():
+    # the current stream is captured, the context's joins it: results come from the graph's own memory, whatever stream they belong to
+    N, K, M = 4, 4096, 3
+    main, side = torch.cuda.Stream(), torch.cuda.Stream()
+    ctx = _context(side, N)
+    opt = lpc.AdamW(ctx, K)
+    U = synth.gradient_vectors(N, K, "gauss", seed=1, device=DEV)
+    X, p, state = torch.ones(M, K, device=DEV), torch.ones(K, device=DEV), opt.init_state()
+    torch.cuda.synchronize()
+    ctx.quantize_pack(U, 0)   # the quantizer plans a layout when it first sees it, and allocates
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=main):
+        side.wait_stream(main)
+        codes, delta, _ = ctx.quantize_pack(U, 1)
+        Y = ctx.packed_matvec(codes, delta, K, X, 0)
+        dX = ctx.packed_matvec_t(codes, delta, K, Y, 0)
+        opt.unpack_average_step(codes, delta, p, state, 1, 0.1)
+        main.wait_stream(side)
+        total = dX.sum()
+        del codes, delta
+        again = Y * 2
+    X.copy_(torch.randn(M, K, device=DEV))
+    torch.cuda.synchronize()
+    for _ in range(3):
+        p.fill_(1), state[0].zero_(), state[1].zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+    torch.cuda.synchronize()
+    got = [t.clone() for t in (Y, dX, again, total, p)]
+    q, fresh = torch.ones(K, device=DEV), opt.init_state()
+    torch.cuda.synchronize()
+    codes, delta, _ = ctx.quantize_pack(U, 1)
+    Y = ctx.packed_matvec(codes, delta, K, X, 0)
+    dX = ctx.packed_matvec_t(codes, delta, K, Y, 0)
+    opt.unpack_average_step(codes, delta, q, fresh, 1, 0.1)
+    ctx.sync_status()
+    for a, b in zip(got, (Y, dX, Y * 2, dX.sum(), q)):
+        assert torch.equal(a, b)
+    del graph
+    opt.close(), ctx.close()
