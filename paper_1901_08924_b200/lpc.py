@@ -346,8 +346,9 @@ class Context:
         assert delta.get_device() == self._device_index and delta.dtype is torch.float32 and delta.is_contiguous()
         assert delta.shape == (rows, -(-cols // group) if group else min(cols, 1))
         assert x.get_device() == self._device_index and dtype in _TYPES and have == need and (have <= 1 or ld[1] == 1)
-        assert not (torch.is_grad_enabled() and (x.requires_grad or delta.requires_grad or (out is not None and out.requires_grad))), "products with packed rows are not recorded for autograd: detach their arguments (packed_matvec_t is the gradient for X)"
         given = out is not None
+        assert not (torch.is_grad_enabled() and (x.requires_grad or delta.requires_grad or (given and out.requires_grad))), \
+            "products with packed rows are not recorded for autograd: detach their arguments (packed_matvec_t is the gradient for X)"
         if not given:
             out = x.new_empty((M, want)) if _current_raw_stream(self._device_index) == self._raw_stream else self._new((M, want), dtype)
             ldo = want
